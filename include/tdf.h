@@ -446,7 +446,7 @@ typedef struct {
   const void* h;            /* device [n_rows x n_cols], as tdf_gated_scan left it              */
   int64_t ld_h;
   const void* dh;           /* device [n_rows x n_cols]: gradient of the objective with respect to h; */
-  int64_t ld_dh;            /* NULL: zeros                                                      */
+  int64_t ld_dh;            /* NULL: zeros (and ld_dh is not looked at)                         */
   const float* dh_last;     /* device float[n_seqs x n_cols]: ... to h_last; NULL: zeros        */
   void* df;                 /* device [n_rows x n_cols], overwritten                            */
   int64_t ld_df;

@@ -756,8 +756,9 @@ extern "C" tdf_status tdf_gated_scan_grad(const tdf_scan* in, const tdf_scan_gra
     if (g->df == g->dx) return refuse(who, "df overlaps dx");
   }
   if (bad_floats(g->dh_last) || bad_floats(g->dh0)) return refuse(who, "dh_last or dh0 is not aligned");
+  // (without dh its window is one row at NULL, all of whose places lie beyond its end)
   ScanArgs a{in->n_rows, in->n_cols, in->n_seqs, in->f, in->ld_f, in->x, in->ld_x, in->offsets, in->h0, const_cast<void*>(g->h), g->ld_h, nullptr,
-             g->dh, g->ld_dh, g->dh_last, g->df, g->ld_df, g->dx, g->ld_dx, g->dh0};
+             g->dh, g->dh ? g->ld_dh : 0, g->dh_last, g->df, g->ld_df, g->dx, g->ld_dx, g->dh0};
   const bool wide = in->n_cols % 4 == 0 && fits(in->f, in->ld_f, size) && fits(in->x, in->ld_x, size) && fits(g->h, g->ld_h, size) &&
                     (!g->dh || fits(g->dh, g->ld_dh, size)) && fits(g->df, g->ld_df, size) && fits(g->dx, g->ld_dx, size) &&
                     ((uintptr_t)in->h0 | (uintptr_t)g->dh_last | (uintptr_t)g->dh0) % 16 == 0;

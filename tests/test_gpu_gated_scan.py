@@ -127,6 +127,28 @@ def test_arguments_left_out(zeros, no_dh, no_last):
     tdf.gated_scan(one[4], one[5], torch.empty_like(one[4]), space(140, 40))
 
 
+@pytest.mark.parametrize("rows", [60, 140, 700])
+@pytest.mark.parametrize("cols", [32, 37])
+@pytest.mark.parametrize("dtype", ref.TYPES, ids=str)
+def test_the_distance_of_rows_that_are_not_given_does_not_matter(dtype, cols, rows):
+    f, x, h0, _, df, dx = make([rows], cols, dtype)
+    h = torch.empty_like(df)
+    tdf.gated_scan(df, dx, h, space(rows, cols), h0=h0.to(DEV))
+    last, ws = torch.randn(1, cols, device=DEV), space(rows, cols)
+    got = []
+    for ld in (0, -1, 3, 1 << 20, 1 << 31, 1 << 62, -(1 << 40)):
+        gf, gx, dh0 = torch.empty_like(df), torch.empty_like(df), torch.empty_like(last)
+        in_ = tdf.Scan(rows, cols, 1, tdf._DTYPES[dtype], df.data_ptr(), cols, dx.data_ptr(), cols, None, None)
+        grads = tdf.ScanGrads(h.data_ptr(), cols, None, ld, last.data_ptr(), gf.data_ptr(), cols, gx.data_ptr(), cols, dh0.data_ptr())
+        assert tdf.lib.tdf_gated_scan_grad(in_, grads, ws.data_ptr(), ws.nbytes, tdf._stream_of(0)) == tdf.OK
+        got.append((gf, gx, dh0))
+    want = ref.scan_grad(f, x, h.cpu(), torch.zeros(rows, cols, dtype=dtype), [0, rows], torch.zeros_like(h0), last.cpu())
+    for g, w, e in zip(got[0][:2], want[:2], want[3:5]):
+        ref.close(g, w, e + ref.half_step(dtype) * (w.abs() + e))
+    ref.close(got[0][2], want[2], want[5])
+    assert all(torch.equal(a, b) for k in got[1:] for a, b in zip(k, got[0]))
+
+
 def test_no_rows():
     e = torch.empty(0, 6, device=DEV)
     off, h0 = torch.zeros(4, dtype=torch.int64, device=DEV), torch.randn(3, 6, device=DEV)
