@@ -457,7 +457,8 @@ typedef struct {
 
 /* Workspace of either direction: device, 256-byte aligned, contents ignored. */
 tdf_status tdf_gated_scan_workspace_size(int64_t n_rows, int64_t n_cols, size_t* bytes);
-/* h_last: device float[n_seqs x n_cols], NULL: not wanted. */
+/* h_last: device float[n_seqs x n_cols], NULL: not wanted.  A state that is carried on has two buffers: h_last that
+ * overlaps h0, or dh0 that overlaps dh_last or h0, is refused. */
 tdf_status tdf_gated_scan(const tdf_scan* in, void* h, int64_t ld_h, float* h_last, void* workspace, size_t workspace_bytes,
                           void* hip_stream);
 tdf_status tdf_gated_scan_grad(const tdf_scan* in, const tdf_scan_grads* grads, void* workspace, size_t workspace_bytes,

@@ -37,6 +37,11 @@ inline const char* bad_matrix(const void* p, int64_t ld, int64_t n_rows, int64_t
   return nullptr;
 }
 inline bool bad_floats(const void* p) { return (uintptr_t)p % 4 != 0; }
+// Two vectors of n floats each, either of which may be NULL, have elements in common.
+inline bool overlap(const void* p, const void* q, int64_t n) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return a && b && (a < b ? b - a : a - b) / sizeof(float) < (uintptr_t)n;
+}
 // The threads of a launch are counted in 32 bits: f(first, count) for runs of at most `most` of n rows.
 constexpr int64_t MOST_WORKGROUPS = 1 << 23;
 template <class F> void in_runs(int64_t n, int64_t most, F&& f) {

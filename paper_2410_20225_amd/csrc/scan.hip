@@ -732,6 +732,8 @@ extern "C" tdf_status tdf_gated_scan(const tdf_scan* in, void* h, int64_t ld_h, 
   if (const char* bad = in->n_rows ? bad_matrix(h, ld_h, in->n_rows, in->n_cols, element_size(in->dtype)) : nullptr) return refuse(who, bad);
   if (bad_floats(h_last)) return refuse(who, "h_last is not aligned");
   if (in->n_rows && (h == in->f || h == in->x)) return refuse(who, "h overlaps an input");
+  // (a tile reads h0 again when another may have written h_last)
+  if (overlap(in->h0, h_last, in->n_seqs * in->n_cols)) return refuse(who, "h_last overlaps h0");
   ScanArgs a{in->n_rows, in->n_cols, in->n_seqs, in->f, in->ld_f, in->x, in->ld_x, in->offsets, in->h0, h, ld_h, h_last};
   const size_t size = element_size(in->dtype);
   const bool wide = in->n_cols % 4 == 0 && fits(in->f, in->ld_f, size) && fits(in->x, in->ld_x, size) && fits(h, ld_h, size) &&
@@ -756,6 +758,8 @@ extern "C" tdf_status tdf_gated_scan_grad(const tdf_scan* in, const tdf_scan_gra
     if (g->df == g->dx) return refuse(who, "df overlaps dx");
   }
   if (bad_floats(g->dh_last) || bad_floats(g->dh0)) return refuse(who, "dh_last or dh0 is not aligned");
+  if (overlap(g->dh_last, g->dh0, in->n_seqs * in->n_cols)) return refuse(who, "dh0 overlaps dh_last");
+  if (overlap(in->h0, g->dh0, in->n_seqs * in->n_cols)) return refuse(who, "dh0 overlaps h0");
   // (without dh its window is one row at NULL, all of whose places lie beyond its end)
   ScanArgs a{in->n_rows, in->n_cols, in->n_seqs, in->f, in->ld_f, in->x, in->ld_x, in->offsets, in->h0, const_cast<void*>(g->h), g->ld_h, nullptr,
              g->dh, g->dh ? g->ld_dh : 0, g->dh_last, g->df, g->ld_df, g->dx, g->ld_dx, g->dh0};

@@ -437,7 +437,8 @@ def _scan(f, x, offsets, h0):
 
 def gated_scan(f, x, h, workspace, offsets=None, h0=None, h_last=None):
     """h_t = sigmoid(f_t) h_(t-1) + (1 - sigmoid(f_t)) x_t over the rows offsets[s] .. offsets[s + 1] - 1 of every sequence s (offsets None:
-    one sequence of all rows), from the state h0[s]; h_last[s] receives the state after the last row."""
+    one sequence of all rows), from the state h0[s]; h_last[s] receives the state after the last row.  A state that is carried from
+    call to call has two buffers: h_last that overlaps h0 is refused, as is dh0 that overlaps dh_last or h0 in gated_scan_grad."""
     in_, like, state = _scan(f, x, offsets, h0)
     gpu = like[2]
     ph, ld_h = _matrix(h, "h", *like)

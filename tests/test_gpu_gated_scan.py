@@ -127,6 +127,22 @@ def test_arguments_left_out(zeros, no_dh, no_last):
     tdf.gated_scan(one[4], one[5], torch.empty_like(one[4]), space(140, 40))
 
 
+def test_states_in_neighbouring_buffers():
+    f, x, h0, offsets, df, dx = make([30, 0, 200], 40, torch.float32)
+    off, ws, h = torch.tensor(offsets, device=DEV), space(230, 40), torch.empty_like(df)
+    both = torch.empty(3, 3, 40, device=DEV)                     # h0, h_last and dh0 beside each other
+    both[0].copy_(h0)
+    tdf.gated_scan(df, dx, h, ws, off, both[0], both[1])
+    tdf.gated_scan_grad(df, dx, h, None, torch.empty_like(df), torch.empty_like(df), ws, off, both[0], both[1], both[2])
+    apart = torch.empty(3, 40, device=DEV)
+    tdf.gated_scan(df, dx, h, ws, off, h0.to(DEV), apart)
+    assert torch.equal(both[1], apart) and torch.equal(both[0].cpu(), h0)
+    with pytest.raises(tdf.TdfError, match="h_last overlaps h0"):
+        tdf.gated_scan(df, dx, h, ws, off, both[0], both[0])
+    with pytest.raises(tdf.TdfError, match="dh0 overlaps dh_last"):
+        tdf.gated_scan_grad(df, dx, h, None, torch.empty_like(df), torch.empty_like(df), ws, off, both[0], both[1], both[1])
+
+
 @pytest.mark.parametrize("rows", [60, 140, 700])
 @pytest.mark.parametrize("cols", [32, 37])
 @pytest.mark.parametrize("dtype", ref.TYPES, ids=str)

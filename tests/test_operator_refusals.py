@@ -169,3 +169,12 @@ def test_the_binding_refuses_tensors_that_the_library_cannot_see_through():
 def test_more_tiles_than_a_launch_has_workgroups():
     refused(tdf.lib.tdf_gated_scan(scan(n_rows=1 << 30, n_cols=100, ld_f=100, ld_x=100), 3 * P, 100, None, 7 * P, 1 << 60, None), "out of range")
     refused(tdf.lib.tdf_gated_scan_grad(scan(n_rows=1 << 24, n_cols=1 << 14, ld_f=1 << 14, ld_x=1 << 14), scan_grads(), 7 * P, 1 << 60, None), "out of range")
+
+
+@pytest.mark.parametrize("off", [0, 4, 60, -4, -60])
+def test_states_that_are_carried_on_have_two_buffers(off):
+    """h0 and dh_last are read while h_last and dh0 are written: 2 sequences of 8 columns, 64 bytes."""
+    refused(tdf.lib.tdf_gated_scan(scan(), 3 * P, 8, P + off, 7 * P, 1 << 30, None), "h_last overlaps h0")
+    refused(tdf.lib.tdf_gated_scan_grad(scan(h0=8 * P), scan_grads(dh_last=P, dh0=P + off), 7 * P, 1 << 30, None), "dh0 overlaps dh_last")
+    refused(tdf.lib.tdf_gated_scan_grad(scan(h0=P), scan_grads(dh_last=8 * P, dh0=P + off), 7 * P, 1 << 30, None), "dh0 overlaps h0")
+    refused(tdf.lib.tdf_gated_scan(scan(n_rows=0), None, 0, P + off, 7 * P, 1 << 30, None), "h_last overlaps h0")
