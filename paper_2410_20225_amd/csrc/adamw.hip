@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(256) k_adamw(AdamArgs a) {
     }
   }
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
-  const float decay = 1.0f - a.plain_lr * t->weight_decay;
+  const float decay = a.plain_lr * t->weight_decay;
   const uint32_t key = mix(a.seed ^ (0x9E3779B9u * (k + 1)));
 #pragma unroll
   for (int j = 0; j < PASSES; ++j) {
@@ -208,7 +208,8 @@ __global__ void __launch_bounds__(256) k_adamw(AdamArgs a) {
       o.m[e] = add(mul(o.m[e], a.beta1), mul(g, a.rest1));
       o.v[e] = add(mul(o.v[e], a.beta2), mul(mul(g, g), a.rest2));
       const float root = fmaf(__builtin_amdgcn_sqrtf(o.v[e]), a.root, a.eps);
-      o.p[e] = fmaf(o.p[e], decay, -(o.m[e] * a.lr) * __builtin_amdgcn_rcpf(root));
+      // (1 - decay would be rounded to a multiple of 2^-24, so that a small decay were none or a larger one, the same way in every step)
+      o.p[e] -= fmaf(o.p[e], decay, o.m[e] * a.lr * __builtin_amdgcn_rcpf(root));
       // (elements that are not there are zeros and stay zeros, unless a NaN scale makes them one, as all of the block)
       tm = max(tm, __float_as_uint(o.m[e]) & 0x7FFFFFFFu);
       tv = max(tv, __float_as_uint(o.v[e]) & 0x7FFFFFFFu);
