@@ -519,7 +519,8 @@ typedef struct {
 
 typedef struct tdf_adamw_plan tdf_adamw_plan; /* opaque, library-owned host object              */
 
-/* The list of tensors, laid out for the kernel; host only.  Refused: tensors one of which writes what another one writes. */
+/* The list of tensors, laid out for the kernel; host only.  Refused: tensors one of which writes what another one writes, and
+ * more than 2^24 - 1 pieces of 4,096 elements of one tensor, the last one rounded up (2^36 elements). */
 tdf_status tdf_adamw_build(const tdf_adamw_tensor* tensors, int64_t n_tensors, tdf_adamw_plan** out);
 void tdf_adamw_destroy(tdf_adamw_plan* plan);
 tdf_status tdf_adamw_workspace_size(const tdf_adamw_plan* plan, size_t* bytes);

@@ -21,6 +21,7 @@ using namespace rows;
 
 constexpr int BLOCK = 128;          // elements that share a scale
 constexpr int64_t CHUNK = 4096;     // elements of a workgroup's piece of a tensor
+constexpr int64_t MOST_CHUNKS = (1 << 24) - 1;   // a workgroup of 256 threads each: less than 2^32 threads
 
 struct AdamTensor {
   int64_t n;
@@ -298,7 +299,7 @@ extern "C" tdf_status tdf_adamw_build(const tdf_adamw_tensor* tensors, int64_t n
                               ((uintptr_t)t.param | (uintptr_t)t.grad | (uintptr_t)t.copy) % 16 == 0 && ((uintptr_t)t.m | (uintptr_t)t.v) % (t.state_bits == 8 ? 8 : 16) == 0, 0});
       const int64_t more = (t.n + CHUNK - 1) / CHUNK;
       chunks += more;
-      if (chunks > (1ll << 31) - 1) return bad("too many elements");
+      if (chunks > MOST_CHUNKS) return bad("too many elements");
       plan.tensor_of.insert(plan.tensor_of.end(), (size_t)more, (uint32_t)k);
     }
     std::sort(written.begin(), written.end());

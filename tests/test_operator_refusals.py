@@ -178,3 +178,13 @@ def test_states_that_are_carried_on_have_two_buffers(off):
     refused(tdf.lib.tdf_gated_scan_grad(scan(h0=8 * P), scan_grads(dh_last=P, dh0=P + off), 7 * P, 1 << 30, None), "dh0 overlaps dh_last")
     refused(tdf.lib.tdf_gated_scan_grad(scan(h0=P), scan_grads(dh_last=8 * P, dh0=P + off), 7 * P, 1 << 30, None), "dh0 overlaps h0")
     refused(tdf.lib.tdf_gated_scan(scan(n_rows=0), None, 0, P + off, 7 * P, 1 << 30, None), "h_last overlaps h0")
+
+
+def test_more_elements_than_a_launch_has_workgroups():
+    huge = dict(param=1 << 45, grad=1 << 46, m=1 << 47, v=1 << 48)
+    most = ((1 << 24) - 1) * 4096
+    refused(build(adam(n=most + 1, **huge))[0], "too many elements")
+    refused(build(adam(n=most, **huge), adam(n=1))[0], "too many elements")
+    st, plan = build(adam(n=most, **huge), adam(n=0))
+    assert st == tdf.OK
+    tdf.lib.tdf_adamw_destroy(plan)
