@@ -231,3 +231,35 @@ def test_another_stream_and_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((y, mean, rstd, dx, dw, db), want))
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES, ids=str)
+@pytest.mark.parametrize("rows,cols", [(65539, 24), (65537, 25), (65538, 96), (65539, 99), (16387, 300), (16385, 301), (16386, 700), (16387, 701), (4099, 1025),
+                                       (4097, 1032), (4098, 1500), (4099, 1501), (4097, 2500)])
+def test_rows_so_many_that_a_thread_has_several(rows, cols, dtype):
+    """More than 4,096 workgroups: several rows of a thread, the last ones not there; rows at whole pieces of 16 bytes and at any element."""
+    w, b = vectors(cols)
+    x, d = make(rows, cols, dtype)
+    y, mean, rstd = forward(x, d, w, b)
+    assert torch.equal(forward(x, d, w, b, y=d)[0], y)               # in place
+    if cols < 400:
+        gradient(*make(rows, cols, dtype), w)
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES, ids=str)
+@pytest.mark.parametrize("cols", [48, 301, 512, 3000, 9000])
+def test_vectors_that_begin_four_bytes_after_an_aligned_place(cols, dtype):
+    w, b = vectors(cols)
+    x, d = make(37, cols, dtype)
+    off_w, off_b = (torch.cat([torch.zeros(1), v]).to(DEV)[1:] for v in (w, b))
+    y = torch.empty_like(d)
+    tdf.layer_norm(d, y, off_w, off_b)
+    want, _, _, e, _, _ = ref.norm(x, w.double(), b.double(), 1e-5)
+    ref.close(y, want, e + ref.half_step(dtype) * (want.abs() + e))
+    mean, rstd = torch.randn(37, device=DEV), torch.rand(37, device=DEV)
+    dy = torch.randn_like(d)
+    got = grads(d, dy, mean, rstd, off_w)
+    want = ref.norm_grad(x, dy.cpu(), mean.cpu(), rstd.cpu(), w.double())
+    ref.close(got[0], want[0], want[3] + ref.half_step(dtype) * (want[0].abs() + want[3]))
+    ref.close(got[1], want[1], want[4])
+    ref.close(got[2], want[2], want[5])
