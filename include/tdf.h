@@ -385,7 +385,7 @@ tdf_status tdf_eval_static(tdf_graph* g, const tdf_inputs* in, tdf_outputs* out,
  *
  *   - The calls enqueue kernels on the caller's stream and return: no synchronisation, no allocation,
  *     no other stream, nothing kept from one call for the next.  They may be recorded into a HIP graph
- *     (tdf_adamw_prepare, a set-up call, may not).  Arguments are checked on the host before anything is
+ *     (tdf_adamw_prepare, a set-up call, may not; a recorded tdf_adamw repeats one step's numbers).  Arguments are checked on the host before anything is
  *     enqueued: TDF_ERR_BAD_ARG, TDF_ERR_WORKSPACE; TDF_ERR_DEVICE where a launch fails.
  *   - A matrix is [n_rows x n_cols] elements of `dtype` (tdf_dtype), row r beginning at element r * ld,
  *     ld >= n_cols: halves of a wider projection's rows are matrices.  Pointers are aligned to their
@@ -436,8 +436,8 @@ typedef struct {
   const void* x;            /* device [n_rows x n_cols]: candidates                             */
   int64_t ld_x;
   const int64_t* offsets;   /* device int64[n_seqs + 1], ascending, within 0 .. n_rows; rows before the first
-                               and from the last one on belong to no sequence: they are not read and
-                               their results not written.  NULL: one sequence of n_rows rows (n_seqs = 1).
+                               and from the last one on belong to no sequence: they may be read, but whatever
+                               they hold changes no result, and their own results are not written.  NULL: one sequence of n_rows rows (n_seqs = 1).
                                Offsets in another order give other results but touch no other memory */
   const float* h0;          /* device float[n_seqs x n_cols], NULL: zeros                       */
 } tdf_scan;
@@ -491,8 +491,8 @@ tdf_status tdf_gated_scan_step(const tdf_scan_step* in, void* hip_stream);
  * value one is taken by a random number that follows from seed, the tensor's place in the list and the
  * element's in the tensor, so that the value is the mean of what is stored; no v above zero is stored as zero.
  * The parameter is changed by the m and v before they are stored.  A scale below 2^-90 is held as zero;
- * where an element of a block is not finite its scale is not, and all of the block's states are NaN
- * in the next step.  States of 32 or 8 bits are zeros before the first step. */
+ * where an m (or v) of a block is not finite its scale is not, and none of the block's m (or v) are finite from the
+ * next step on: NaN, or infinite where the scale is infinite and the stored number not zero.  States of 32 or 8 bits are zeros before the first step. */
 typedef struct {
   int64_t n;                /* elements; 0: nothing to do                                       */
   int32_t param_dtype;      /* tdf_dtype; bf16 parameters are rounded to nearest in every step  */
@@ -513,7 +513,8 @@ typedef struct {
   double lr, beta1, beta2, eps;   /* betas in [0, 1)                                            */
   int64_t step;             /* >= 1                                                             */
   const float* grad_scale;  /* device float[1], read when the kernel runs; NULL: 1              */
-  uint32_t seed;            /* of the random numbers; another one in every step                 */
+  uint32_t seed;            /* of the random numbers; another one in every step, `step` for instance: with the
+                               same one an element is rounded to the same side each time, and 8-bit states drift */
   uint32_t reserved;        /* 0                                                                */
 } tdf_adamw_step;
 
@@ -527,7 +528,8 @@ tdf_status tdf_adamw_workspace_size(const tdf_adamw_plan* plan, size_t* bytes);
 /* Copies the list into the workspace (device, 256-byte aligned), which belongs to the plan from then on; waits for
  * the stream.  Once per plan, with the device current on which the steps run. */
 tdf_status tdf_adamw_prepare(tdf_adamw_plan* plan, void* workspace, size_t workspace_bytes, void* hip_stream);
-/* One step.  (A recorded one repeats the same `step` and `seed`.) */
+/* One step.  Its numbers are those of the call: recorded into a HIP graph, every replay repeats the same step, learning
+ * rate and seed, so a graph of a training step leaves it out, and the call follows the replay. */
 tdf_status tdf_adamw(const tdf_adamw_plan* plan, const tdf_adamw_step* step, void* hip_stream);
 #endif /* __HIPCC_RTC__ */
 

@@ -12,8 +12,8 @@ namespace {
 using namespace rows;
 
 // a = sigmoid(f) = 1 / (1 + E) and keep = 1 - a = a E with E = exp(-f): both have a small relative error wherever f lies.  E ends at
-// 2^126, so that a E is 1 there.  bf16: the hardware's exponential and reciprocal as they are, a few 2^-24 off.  fp32: the exponential's
-// argument with the bits that its product loses, and a Newton step for the reciprocal.
+// 2^126, so that a E is 1 there.  bf16: the hardware's exponential and reciprocal as they are, a few 2^-24 off, and E up to |f| 2^-24
+// more, since the exponential's argument is rounded.  fp32: the argument with the bits that its product loses, and a Newton step for the reciprocal.
 template <int DT> __device__ __forceinline__ void gate(float f, float& a, float& keep) {
   constexpr float LOG2E = 1.44269504088896340736f, LOW = 1.92596299112661746887e-8f;   // log2(e) and what that leaves of it
   if constexpr (DT == TDF_BF16) {
@@ -68,7 +68,7 @@ constexpr int TICKET_APART = 32;  // counters: a line each
 // each of the PARTS parts of the workgroup L rows one after the other, whose elements are all in flight together.  L is eight; four for the
 // gradients in fp32, whose elements would take all registers.
 constexpr int VEC = 4, LANES = 16, COLS = LANES * VEC, PARTS = THREADS / LANES;
-constexpr int WAVES = THREADS / 64, SUBS = 64 / LANES;   // waves of a workgroup, parts of a wave
+constexpr int WAVES = THREADS / 64;                      // of a workgroup
 constexpr int length(int dt, bool back) { return dt == TDF_F32 && back ? 4 : 8; }
 constexpr int rows_of(int dt, bool back) { return PARTS * length(dt, back); }
 constexpr int MOST_ROWS_OF = 128, LEAST_ROWS_OF = 64;    // of a tile
@@ -525,7 +525,9 @@ template <int DT, bool LOOSE, bool BACK, bool CHAINED> struct Tile {
   }
 };
 
-// Workgroups of a compute unit that the registers leave room for.
+// Workgroups that a compute unit is to have room for, and the registers of a wave that this leaves.  Rows at whole four elements need no
+// more than these (79 of 80 in bf16, 104 to 112 of 128 otherwise).  Rows at any element keep scalars in vector registers (20 to 32 in three of
+// four kernels), and results in bf16 five vector registers in scratch, 16 bytes a lane; fewer workgroups for these have not been measured.
 constexpr int wgs_wanted(int dt, bool back) { return dt == TDF_BF16 ? (back ? 4 : 6) : (back ? 4 : 4); }
 
 // Several tiles of rows: every workgroup takes one ticket.  What bounds it is how long tiles are under way, waits for those before them among

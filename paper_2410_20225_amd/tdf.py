@@ -522,9 +522,9 @@ def adamw_prepare(plan, workspace):
 
 def adamw(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, seed=None, grad_scale=None):
     """One AdamW step over the plan's tensors, the step-th (from 1).  seed: of the random rounding of 8-bit states, another one in
-    every step (with the same one an element is rounded to the same side every time, and its states drift away); None: step's lowest 32
-    bits.  grad_scale: a float32 on the GPU that the gradients are multiplied by.  Recorded into a graph, a replay repeats the
-    same step, learning rate and seed."""
+    every step (with the same one an element is rounded to the same side every time, and 8-bit states drift); None: the step.
+    grad_scale: a float32 on the GPU that the gradients are multiplied by.  Recorded into a graph, a replay repeats the same step,
+    learning rate and seed."""
     in_ = AdamwStep(lr, beta1, beta2, eps, step, None if grad_scale is None else _vector(grad_scale.reshape(1), "grad_scale", (1,), plan.gpu),
                     step if seed is None else seed, 0)
     _done(plan.lib.tdf_adamw(plan.handle, in_, _stream_of(plan.gpu)), "tdf_adamw")
