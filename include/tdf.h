@@ -385,8 +385,8 @@ tdf_status tdf_eval_static(tdf_graph* g, const tdf_inputs* in, tdf_outputs* out,
  *
  *   - The calls enqueue kernels on the caller's stream and return: no synchronisation, no allocation,
  *     no other stream, nothing kept from one call for the next.  They may be recorded into a HIP graph
- *     (tdf_adamw_prepare, a set-up call, may not; a recorded tdf_adamw repeats one step's numbers).  Arguments are checked on the host before anything is
- *     enqueued: TDF_ERR_BAD_ARG, TDF_ERR_WORKSPACE; TDF_ERR_DEVICE where a launch fails.
+ *     (tdf_adamw_prepare, a set-up call, may not; a recorded tdf_adamw repeats one step's numbers).
+ *     Arguments are checked on the host before anything is enqueued: TDF_ERR_BAD_ARG, TDF_ERR_WORKSPACE; TDF_ERR_DEVICE where a launch fails.
  *   - A matrix is [n_rows x n_cols] elements of `dtype` (tdf_dtype), row r beginning at element r * ld,
  *     ld >= n_cols: halves of a wider projection's rows are matrices.  Pointers are aligned to their
  *     elements; where bases and ld are multiples of 16 bytes, loads are wide.  Element offsets are 64 bits.
@@ -492,7 +492,8 @@ tdf_status tdf_gated_scan_step(const tdf_scan_step* in, void* hip_stream);
  * element's in the tensor, so that the value is the mean of what is stored; no v above zero is stored as zero.
  * The parameter is changed by the m and v before they are stored.  A scale below 2^-90 is held as zero;
  * where an m (or v) of a block is not finite its scale is not, and none of the block's m (or v) are finite from the
- * next step on: NaN, or infinite where the scale is infinite and the stored number not zero.  States of 32 or 8 bits are zeros before the first step. */
+ * next step on: NaN, or infinite where the scale is infinite and the stored number not zero.  States of 32 or 8 bits
+ * are zeros before the first step. */
 typedef struct {
   int64_t n;                /* elements; 0: nothing to do                                       */
   int32_t param_dtype;      /* tdf_dtype; bf16 parameters are rounded to nearest in every step  */

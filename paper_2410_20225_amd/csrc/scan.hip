@@ -526,7 +526,7 @@ template <int DT, bool LOOSE, bool BACK, bool CHAINED> struct Tile {
 };
 
 // Workgroups that a compute unit is to have room for, and the registers of a wave that this leaves.  Rows at whole four elements need no
-// more than these (79 of 80 in bf16, 104 to 112 of 128 otherwise).  Rows at any element keep scalars in vector registers (20 to 32 in three of
+// more than these (79 of 80 for results in bf16, 104 to 112 of 128 in the others).  Rows at any element keep scalars in vector registers (20 to 32 in three of
 // four kernels), and results in bf16 five vector registers in scratch, 16 bytes a lane; fewer workgroups for these have not been measured.
 constexpr int wgs_wanted(int dt, bool back) { return dt == TDF_BF16 ? (back ? 4 : 6) : (back ? 4 : 4); }
 
